@@ -8,9 +8,16 @@
 
 #include "ejoin.h"
 
+// Words of a status block.  0 .. 3 and 8 .. 15 are the joins' (see k_reset); of the context's own block, two more that no join kernel reads or
+// clears by itself: the pair counter of a join that is returned in batches, and what was wrong with tokens (ejoin_embed_status).
+constexpr int EJ_STATUS_WORDS = 64;
+constexpr int EJ_BATCH_COUNTER = 32;  // 64 bits: 32 and 33
+constexpr int EJ_TOKEN_STATUS = 48;
+static_assert(EJ_TOKEN_STATUS >= EJ_BATCH_COUNTER + 2 && EJ_TOKEN_STATUS < EJ_STATUS_WORDS, "words of their own");
+
 // Device memory one call works in: either the context's own (grown on demand) or a carving of the static scratch.
 struct Workspace {
-  uint32_t* status;  // status block, 64 words (see k_reset)
+  uint32_t* status;  // status block, EJ_STATUS_WORDS words (see below and k_reset)
   float* s;          // norms (4 B per point)
   uint32_t* maxima;  // behind them, small problems and the dense-tile call: largest norms of the norm kernels' workgroups (at most one per NORM_POINTS points)
   uint4* Xp;         // packed copy of X plus the augmentation k-block
@@ -38,12 +45,11 @@ struct ejoin_ctx {
   // ejoin_embed.h: memory its calls work in, grown on demand, and the device word in which they leave what was wrong with tokens
   unsigned char* embed;
   int64_t embed_bytes;
-  uint32_t* token_status;  // word EJ_TOKEN_STATUS of the status block: no join writes it
+  uint32_t* token_status;  // word EJ_TOKEN_STATUS of the context's own status block
   uint32_t* tickets;       // device: EJ_TICKETS counters, all zero between calls
   char hip_error[256];
 };
 
-constexpr int EJ_TOKEN_STATUS = 32;
 constexpr int EJ_TICKETS = 4096;
 
 // What the kernels of f8.hip need once on a device, which is current.

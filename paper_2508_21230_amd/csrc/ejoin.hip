@@ -119,12 +119,12 @@ struct JoinArgs {
 // ------------------------------------------------------------------------------------------
 // Small kernels
 // ------------------------------------------------------------------------------------------
-// Status block of a workspace (64 words): [0] status word, [1] largest norm seen so far in the call (FP32 bits),
+// Status block of a workspace (EJ_STATUS_WORDS words): [0] status word, [1] largest norm seen so far in the call (FP32 bits),
 // [2..3] the constant C = { c, c, c, 0 } of the call's augmentation step (FP16 bits, written by k_aux),
 // [8..15] alignment counters of the XCDs.  Between calls [1] and [8..15] are zero: k_aux clears the counters
 // (and the result counter of the call), k_join clears the maximum.  k_reset restores that state after a call
 // that did not get as far as its join kernel, and before every call of k_join on the shared static workspace.
-// (Small problems and the dense-tile call use word [0] only.)
+// (Small problems and the dense-tile call use word [0] only.)  The context's own block holds two words more, EJ_BATCH_COUNTER and EJ_TOKEN_STATUS.
 __global__ void k_reset(uint32_t* status_and_max) {
   if (threadIdx.x < 8) status_and_max[8 + threadIdx.x] = 0;
   if (threadIdx.x == 0) {
@@ -3868,8 +3868,8 @@ int ejoin_create(ejoin_ctx** out, int device) {
     delete ctx;
     return EJOIN_EHIP;
   }
-  hipError_t e = hipMalloc(reinterpret_cast<void**>(&ctx->ws.status), 256);
-  if (e == hipSuccess) e = hipMemset(ctx->ws.status, 0, 256);
+  hipError_t e = hipMalloc(reinterpret_cast<void**>(&ctx->ws.status), EJ_STATUS_WORDS * sizeof(uint32_t));
+  if (e == hipSuccess) e = hipMemset(ctx->ws.status, 0, EJ_STATUS_WORDS * sizeof(uint32_t));
   for (int rf : {2, 4, 8, 16})
     for (FewKernel kernel : {few_kernel<false>(rf), few_kernel<true>(rf)})
       if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
@@ -3997,7 +3997,7 @@ int ejoin_selfjoin_pairs_to_host(ejoin_ctx* ctx, const uint16_t* X, int64_t n, i
     bounds[nb] = 0xFFFFFFFFu;
   }
   // the counter lives in the context's status block (the caller gets the final count in host memory)
-  uint64_t* counter = reinterpret_cast<uint64_t*>(ctx->ws.status + 32);
+  uint64_t* counter = reinterpret_cast<uint64_t*>(ctx->ws.status + EJ_BATCH_COUNTER);
   EJ_RC(ensure_workspace(ctx, pad_rows(n), pad_dims(d)));
   EJ_RC(run_join<false>(ctx, ctx->ws, true, X, n, ld, nullptr, 0, 0, d, eps, pair_results(pairs, dist2, capacity, counter), st, bounds, nb));
   // As each batch completes, its pairs go to the host on the copy stream while the next batch computes.
