@@ -111,7 +111,9 @@ int ejoin_embed_status(ejoin_ctx* ctx, int* status);
 /* Each call works in at most 16 KiB + 16 * t bytes of the context's memory, where rows are not cut into pieces (few or very long ones are) in none. */
 int ejoin_distill(ejoin_ctx* ctx, const void* Z, int32_t ztype, int64_t t, int64_t v, int64_t ldz, const void* ids, int32_t id_type, const float* teacher,
                   int32_t k, int64_t ldi, float temperature, float* loss, float* lse, void* stream);
-/* The gradient, from the lse of the forward call (what a differentiation engine keeps). */
+/* The gradient, from the lse of the forward call (what a differentiation engine keeps).  q is exp(Z / T - lse), so it carries the rounding of
+ * an lse in FP32: a factor of exp(|lse| 2^-24), 1.00006 at an lse of 1,000, and anything between 0 and v where |lse| passes 2^24 (a row that holds
+ * the type's lowest value throughout).  ejoin_distill_with_grad goes by (largest score, sum) and has no such limit. */
 int ejoin_distill_grad(ejoin_ctx* ctx, const void* Z, int32_t ztype, int64_t t, int64_t v, int64_t ldz, const float* lse, const void* ids, int32_t id_type,
                        const float* teacher, int32_t k, int64_t ldi, const float* weights, float temperature, void* dZ, int64_t lddz, void* stream);
 /* Loss and gradient in one call, Z read once but for few rows of more than 53,248 scores and rows that no workgroup's registers hold. */

@@ -5,6 +5,8 @@
 // difference comes first: scores as large as FP32 holds (masks) leave no more error in it than others.
 //   loss = T^2 sum_k p_k (log p_k - log q_k),  p the softmax of the list's logits / T over its entries;  dz_v = weight T (q_v - sum of the p_k with id v)
 // A row without entries has no loss and a gradient of zeros.
+#include <type_traits>
+
 #include "embed.h"
 
 namespace {
@@ -49,7 +51,8 @@ struct DistillArgs {
   float* lse;
   void* dZ;
   int64_t lddz;
-  Stats* parts;  // long rows: t x splits
+  Stats* parts;      // long rows: t x splits
+  Stats* row_stats;  // ... joined, for the gradient of the same call; may be null
   uint32_t* tickets;
   uint32_t splits;
   int64_t per_split;  // scores, a multiple of eight
@@ -120,14 +123,17 @@ __device__ __forceinline__ float divergence(const DistillArgs& a, int64_t row, c
   return sum_wave(sum);
 }
 
-// weight * q of a score: from the row's statistics, or from its lse.
+// weight * q of a score: from the row's statistics, or from its lse.  An lse in 32 bits holds the sum only to 2^-24 of its own magnitude: what it
+// gives is as far off as exp(|lse| 2^-24) is from one, so a call that has the statistics goes by those.
 struct FromStats {
   float top, c, factor;
+  static __device__ __forceinline__ Stats of_row(const DistillArgs& a, int64_t row) { return a.row_stats[row]; }
   __device__ FromStats(const DistillArgs& a, Stats s, float weight) : top(s.top == -INFINITY ? 0.f : s.top), c(a.c), factor(nothing(s) ? 0.f : weight / s.sum) {}
   __device__ __forceinline__ float operator()(float z) const { return factor * exp2_of((z - top) * c); }
 };
 struct FromLse {
   float lse, inv_t, factor;
+  static __device__ __forceinline__ float of_row(const DistillArgs& a, int64_t row) { return a.lse_in[row]; }
   __device__ FromLse(const DistillArgs& a, float lse_, float weight) : lse(lse_ == -INFINITY ? 0.f : lse_), inv_t(a.inv_t), factor(lse_ == -INFINITY ? 0.f : weight) {}
   __device__ __forceinline__ float operator()(float z) const { return factor * exp2_of((z * inv_t - lse) * LOG2E); }
 };
@@ -252,7 +258,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREA
     const float weight = a.weights[row] * a.temperature;
     auto weighted_q = [&] {
       if constexpr (FORWARD) return FromStats(a, s, weight);
-      else return FromLse(a, a.lse_in[row], weight);
+      else return FromLse(a, FromLse::of_row(a, row), weight);
     }();
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) {
@@ -340,11 +346,13 @@ __global__ __launch_bounds__(LONG_THREADS + 64) void k_distill_long(const Distil
   const float loss = list_lse == -INFINITY ? 0.f : a.temperature * a.temperature * divergence(a, row, list, list_lse, s);
   if (lane == 0) {
     a.loss[row] = loss;
-    a.lse[row] = lse_of(s, a.inv_t);
+    if (a.lse) a.lse[row] = lse_of(s, a.inv_t);
+    if (a.row_stats) a.row_stats[row] = s;
   }
 }
 
-template <typename T>
+// FROM: FromStats after k_distill_long of the same call, FromLse where the caller kept an lse.
+template <typename T, typename FROM>
 __global__ __launch_bounds__(LONG_THREADS) void k_distill_long_grad(const DistillArgs a) {
   __shared__ List list;
   __shared__ float shared_list_lse;
@@ -357,7 +365,7 @@ __global__ __launch_bounds__(LONG_THREADS) void k_distill_long_grad(const Distil
     if (threadIdx.x == 0) shared_list_lse = list_lse;
   }
   const float weight = a.weights[row] * a.temperature;
-  const FromLse weighted_q(a, a.lse_in[row], weight);
+  const FROM weighted_q(a, FROM::of_row(a, row), weight);
   __syncthreads();  // (the entries' scores are read before any is overwritten: dZ may be Z)
   if (shared_list_lse == -INFINITY) {  // no entry: zeros
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -450,15 +458,14 @@ int launch_distill(ejoin_ctx* ctx, DistillArgs& a, int32_t ztype, hipStream_t st
     const dim3 grid((unsigned)(a.t * a.splits));
     if (FORWARD) {
       const int64_t parts = up(a.t * a.splits * (int64_t)sizeof(Stats), 256);
-      rc = ensure_embed(ctx, parts + a.t * 4);
+      rc = ensure_embed(ctx, parts + (GRAD ? a.t * (int64_t)sizeof(Stats) : 0));
       if (rc != EJOIN_OK) return;
       a.parts = reinterpret_cast<Stats*>(ctx->embed);
       a.tickets = ctx->tickets;
-      if (!a.lse) a.lse = reinterpret_cast<float*>(ctx->embed + parts);
+      if (GRAD) a.row_stats = reinterpret_cast<Stats*>(ctx->embed + parts);
       hipLaunchKernelGGL(k_distill_long<T>, grid, dim3(LONG_THREADS + 64), 0, st, a);
-      a.lse_in = a.lse;
     }
-    if (GRAD) hipLaunchKernelGGL(k_distill_long_grad<T>, grid, dim3(LONG_THREADS), 0, st, a);
+    if constexpr (GRAD) hipLaunchKernelGGL((k_distill_long_grad<T, std::conditional_t<FORWARD, FromStats, FromLse>>), grid, dim3(LONG_THREADS), 0, st, a);
   });
   if (rc != EJOIN_OK) return rc;
   EJ_TRY(hipGetLastError());
