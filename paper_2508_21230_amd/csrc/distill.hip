@@ -80,16 +80,20 @@ __device__ __forceinline__ float sum_wave(float x) {
   return x;
 }
 
+// Of a list's logits: the largest, -infinity where there is no entry, and log sum exp((logit - top) / T).  As with the scores the difference comes first.
+struct ListStats {
+  float top, log_sum;
+};
+
 // One wavefront fills the list (ids outside [from, to) too: the probabilities are those of all entries, the scores only of those inside).
-// The log of the sum of the entries' exponentials, -infinity where there is no entry.
 template <typename T>
-__device__ __forceinline__ float fill_list(const DistillArgs& a, int64_t row, const T* z, int64_t from, int64_t to, List& list) {
+__device__ __forceinline__ ListStats fill_list(const DistillArgs& a, int64_t row, const T* z, int64_t from, int64_t to, List& list) {
   const int lane = threadIdx.x & 63;
   const float* teacher = a.teacher + row * a.ldi;
   float top = -INFINITY;
   for (int i = lane; i < a.k; i += 64) {
     const int64_t id = a.id_type == EJOIN_I64 ? static_cast<const int64_t*>(a.ids)[row * a.ldi + i] : static_cast<const int32_t*>(a.ids)[row * a.ldi + i];
-    const float u = teacher[i] * a.inv_t;
+    const float u = teacher[i];
     const bool there = id >= 0 && id < a.v && u != -INFINITY;
     if (id < -1 || id >= a.v) *a.status = EJOIN_STATUS_TOKEN;
     list.id[i] = there ? (int32_t)id : -1;
@@ -98,17 +102,17 @@ __device__ __forceinline__ float fill_list(const DistillArgs& a, int64_t row, co
     if (there) top = fmaxf(top, u != u ? INFINITY : u);  // (NaN: the exponentials below make it one)
   }
   top = max_wave(top);
-  if (top == -INFINITY) return top;
+  if (top == -INFINITY) return {top, 0.f};
   float sum = 0.f;
   for (int i = lane; i < a.k; i += 64)  // (a lane reads what it wrote)
-    if (list.id[i] >= 0) sum += exp2_of((list.p[i] - top) * LOG2E);
+    if (list.id[i] >= 0) sum += exp2_of((list.p[i] - top) * a.c);
   sum = sum_wave(sum);
-  for (int i = lane; i < a.k; i += 64) list.p[i] = list.id[i] >= 0 ? exp2_of((list.p[i] - top) * LOG2E) / sum : 0.f;
-  return top + logf(sum);
+  for (int i = lane; i < a.k; i += 64) list.p[i] = list.id[i] >= 0 ? exp2_of((list.p[i] - top) * a.c) / sum : 0.f;
+  return {top, logf(sum)};
 }
 
 // sum_i p_i (log p_i - log q_i) of a row with entries, by the wavefront that filled the list for all of the row.
-__device__ __forceinline__ float divergence(const DistillArgs& a, int64_t row, const List& list, float list_lse, Stats s) {
+__device__ __forceinline__ float divergence(const DistillArgs& a, int64_t row, const List& list, ListStats l, Stats s) {
   const int lane = threadIdx.x & 63;
   const float* teacher = a.teacher + row * a.ldi;
   const float log_sum = logf(s.sum);
@@ -118,7 +122,7 @@ __device__ __forceinline__ float divergence(const DistillArgs& a, int64_t row, c
     const float z = list.z[i], p = list.p[i];
     const float log_q = z == -INFINITY && s.sum == s.sum ? -INFINITY : (z - s.top) * a.inv_t - log_sum;
     // (an entry whose probability is zero to 32 bits adds nothing, unless the row's loss is NaN anyway)
-    sum += p == 0.f && log_q == log_q ? 0.f : p * (teacher[i] * a.inv_t - list_lse - log_q);
+    sum += p == 0.f && log_q == log_q ? 0.f : p * ((teacher[i] - l.top) * a.inv_t - l.log_sum - log_q);
   }
   return sum_wave(sum);
 }
@@ -190,7 +194,7 @@ template <typename T, int THREADS, int PIECES, bool FORWARD, bool GRAD>
 __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREADS * PIECES * (int)sizeof(T) > 512 * 12 * 2 ? 4 : 2) void k_distill_row(const DistillArgs a) {
   __shared__ List list;
   __shared__ Stats wave_stats[THREADS / 64];
-  __shared__ float shared_list_lse;
+  __shared__ float shared_list_top;
   const int64_t row = blockIdx.x;
   const T* z = static_cast<const T*>(a.Z) + row * a.ldz;
   const uint32_t v = (uint32_t)a.v, whole = v & ~7u, mine = threadIdx.x * 8;
@@ -207,10 +211,10 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREA
   const bool odd = threadIdx.x < v - whole;  // the up to seven scores past the last eight: one a thread
   const uint32_t odd_at = whole + threadIdx.x;
   const float rest = odd ? Element<T>::get(z[odd_at]) : -INFINITY;
-  float list_lse = 0.f;
+  ListStats l{0.f, 0.f};
   if (threadIdx.x < 64) {
-    list_lse = fill_list(a, row, z, 0, a.v, list);
-    if (threadIdx.x == 0) shared_list_lse = list_lse;
+    l = fill_list(a, row, z, 0, a.v, list);
+    if (threadIdx.x == 0) shared_list_top = l.top;
   }
   Stats s{-INFINITY, 0.f};
   if (FORWARD) {
@@ -240,7 +244,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREA
 #pragma unroll
     for (int w = 1; w < THREADS / 64; ++w) s = merge(s, wave_stats[w], a.c);
     if (threadIdx.x < 64) {
-      const float loss = list_lse == -INFINITY ? 0.f : a.temperature * a.temperature * divergence(a, row, list, list_lse, s);
+      const float loss = l.top == -INFINITY ? 0.f : a.temperature * a.temperature * divergence(a, row, list, l, s);
       if (threadIdx.x == 0) {
         a.loss[row] = loss;
         if (a.lse) a.lse[row] = lse_of(s, a.inv_t);
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREA
   }
   if constexpr (GRAD) {
     T* dz = static_cast<T*>(a.dZ) + row * a.lddz;
-    if (shared_list_lse == -INFINITY) {  // no entry: zeros
+    if (shared_list_top == -INFINITY) {  // no entry: zeros
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       for (uint32_t at = mine; at < whole; at += THREADS * 8) store8<T, true>(dz + at, zero);
       if (odd) dz[odd_at] = Element<T>::put(0.f);
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(LONG_THREADS + 64) void k_distill_long(const Distil
     s = merge_wave(s, a.c);
     if (lane == 0) wave_stats[threadIdx.x >> 6] = s;
   }
-  const float list_lse = threadIdx.x < LONG_THREADS ? 0.f : fill_list(a, row, z, 0, a.v, list);
+  const ListStats l = threadIdx.x < LONG_THREADS ? ListStats{0.f, 0.f} : fill_list(a, row, z, 0, a.v, list);
   __syncthreads();
   if (threadIdx.x < LONG_THREADS) return;
   s = lane < LONG_THREADS / 64 ? wave_stats[lane] : Stats{-INFINITY, 0.f};
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(LONG_THREADS + 64) void k_distill_long(const Distil
       s = merge(s, __builtin_bit_cast(Stats, __hip_atomic_load(parts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)), a.c);
     s = merge_wave(s, a.c);
   }
-  const float loss = list_lse == -INFINITY ? 0.f : a.temperature * a.temperature * divergence(a, row, list, list_lse, s);
+  const float loss = l.top == -INFINITY ? 0.f : a.temperature * a.temperature * divergence(a, row, list, l, s);
   if (lane == 0) {
     a.loss[row] = loss;
     if (a.lse) a.lse[row] = lse_of(s, a.inv_t);
@@ -355,19 +359,19 @@ __global__ __launch_bounds__(LONG_THREADS + 64) void k_distill_long(const Distil
 template <typename T, typename FROM>
 __global__ __launch_bounds__(LONG_THREADS) void k_distill_long_grad(const DistillArgs a) {
   __shared__ List list;
-  __shared__ float shared_list_lse;
+  __shared__ float shared_list_top;
   const int64_t row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
   const T* z = static_cast<const T*>(a.Z) + row * a.ldz;
   const int64_t from = split * a.per_split, to = from + a.per_split < a.v ? from + a.per_split : a.v;
   T* dz = static_cast<T*>(a.dZ) + row * a.lddz;
   if (threadIdx.x < 64) {
-    const float list_lse = fill_list(a, row, z, from, to, list);
-    if (threadIdx.x == 0) shared_list_lse = list_lse;
+    const ListStats l = fill_list(a, row, z, from, to, list);
+    if (threadIdx.x == 0) shared_list_top = l.top;
   }
   const float weight = a.weights[row] * a.temperature;
   const FROM weighted_q(a, FROM::of_row(a, row), weight);
   __syncthreads();  // (the entries' scores are read before any is overwritten: dZ may be Z)
-  if (shared_list_lse == -INFINITY) {  // no entry: zeros
+  if (shared_list_top == -INFINITY) {  // no entry: zeros
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int64_t at = from + threadIdx.x * 8; at < to; at += LONG_THREADS * 8) store8(dz + at, to - at < 8 ? (int)(to - at) : 8, zero);
     return;

@@ -27,8 +27,9 @@ def ej():
 
 
 def definition(z, ids, teacher, weights, T):
-    u, tl = z.double() / T, teacher.double() / T
     there = (ids >= 0) & (teacher != -torch.inf)
+    u = z.double() / T
+    tl = (teacher.double() - teacher.double().amax(dim=1, keepdim=True)) / T  # (the difference first: 64 bits do not hold 3e38 + log 7 either)
     some = there.any(dim=1)
     at = ids.clamp(min=0).long()
     log_q = torch.log_softmax(u, dim=1)
