@@ -106,7 +106,7 @@ int ejoin_embed_status(ejoin_ctx* ctx, int* status);
  * -infinity all q are 0.
  *   Z, dZ    t x v, row strides ldz, lddz, both of type ztype; dZ may be Z
  *   ids      t x k, row stride ldi;  teacher FP32, t x k, row stride ldi
- *   0 <= k <= EJOIN_DISTILL_MAX_ENTRIES;  1 <= v < 2^31;  t = 0 enqueues nothing;  temperature > 0 and finite */
+ *   0 <= k <= EJOIN_DISTILL_MAX_ENTRIES;  1 <= v < 2^31;  t = 0 enqueues nothing;  temperature finite and at least 4.24e-39 (log2(e) / T is finite) */
 #define EJOIN_DISTILL_MAX_ENTRIES 1024
 /* Each call works in at most 16 KiB + 16 * t bytes of the context's memory, where rows are not cut into pieces (few or very long ones are) in none. */
 int ejoin_distill(ejoin_ctx* ctx, const void* Z, int32_t ztype, int64_t t, int64_t v, int64_t ldz, const void* ids, int32_t id_type, const float* teacher,

@@ -396,9 +396,12 @@ __global__ __launch_bounds__(LONG_THREADS) void k_distill_long_grad(const Distil
 }
 
 // ------------------------------------------------------------------------------------------ host side
+// log2(e) / T: exp(x / T) = 2^(c x).
+float base2(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
+
 bool bad_args(const ejoin_ctx* ctx, int32_t ztype, int64_t t, int64_t v, int64_t ldz, int32_t id_type, int32_t k, int64_t ldi, float temperature) {
   if (!ctx || bad_type(ztype) || (id_type != EJOIN_I32 && id_type != EJOIN_I64) || t < 0 || t >= (1ll << 31) || v < 1 || v >= (1ll << 31) || ldz < v) return true;
-  return k < 0 || k > MOST_ENTRIES || ldi < k || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature);
+  return k < 0 || k > MOST_ENTRIES || ldi < k || !(temperature > 0.f) || !isfinite(temperature) || !isfinite(base2(temperature));
 }
 
 typedef void (*DistillKernel)(DistillArgs);
@@ -482,7 +485,7 @@ DistillArgs distill_args(ejoin_ctx* ctx, const void* Z, int64_t t, int64_t v, in
   memset(&a, 0, sizeof(a));
   a.Z = Z, a.t = t, a.v = v, a.ldz = ldz, a.ids = ids, a.id_type = id_type, a.teacher = teacher, a.k = k, a.ldi = ldi;
   a.inv_t = 1.f / temperature;
-  a.c = (float)(1.4426950408889634 / (double)temperature);
+  a.c = base2(temperature);
   a.temperature = temperature;
   a.status = ctx->token_status;
   return a;

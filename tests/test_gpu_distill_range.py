@@ -35,3 +35,17 @@ def test_lists_of_large_logits(ej, t, v, T):
     grad = ej.distill_grad(z, lse, ids, teacher, weights, temperature=T)
     slack = weights[:, None] * T * torch.exp(z.double() / T - lse.double()[:, None]) * 2.0 ** -23 * (2 * lse.double().abs()[:, None] + 2 * z.double().abs() / T + 4)
     assert ((grad.double() - want).abs() <= off + slack).all()
+
+
+def test_temperatures_at_the_ends_of_the_range(ej):
+    """1 / T times log2 e has to be a number that FP32 holds; every T from there on gives one."""
+    z = torch.zeros((2, 40), device="cuda")
+    ids, teacher, weights = torch.zeros((2, 1), dtype=torch.int32, device="cuda"), torch.zeros((2, 1), device="cuda"), torch.ones(2, device="cuda")
+    for T in (3e-39, 4.2e-39):
+        with pytest.raises(pkg.EJoinError):
+            ej.distill(z, ids, teacher, temperature=T)
+        with pytest.raises(pkg.EJoinError):
+            ej.distill_with_grad(z, ids, teacher, weights, temperature=T)
+    for T in (4.3e-39, 1e-30, 1e18):
+        _, lse = ej.distill(z, ids, teacher, temperature=T)
+        assert torch.allclose(lse.cpu(), torch.full((2,), 40.0).log())
