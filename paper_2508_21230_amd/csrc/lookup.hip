@@ -81,12 +81,18 @@ constexpr int SORT_THREADS = 512;  // (as many as there are digits)
 constexpr int SORT_ITEMS = 4;
 constexpr int SORT_BLOCK = SORT_THREADS * SORT_ITEMS;
 constexpr int CHUNK = 32;
+// From SCAN_FROM blocks on their counts are turned into running sums first, in groups of SCAN_BLOCKS; below, every block adds up the counts of all
+// others for itself, which is two launches less but grows as their square.  The gradient of 400,000, 500,000, 600,000 and 4,000,000 tokens of 100,000
+// rows of 64 with running sums 74, 77, 84 and 404 us, without 71, 77, 92 and 963; of 300 rows of 16 57, 60, 64, 169 and 54, 59, 67, 444.
+constexpr int SCAN_BLOCKS = 128;
+constexpr int SCAN_FROM = 256;
 
 struct SortArgs {
   const void* tokens;  // first pass
   const uint2* items;  // (key, place)
   uint2* items_out;
-  uint32_t* counts;  // of the blocks, DIGITS each
+  uint32_t* counts;  // of the blocks, DIGITS each; scanned: what the blocks before each in its group have
+  uint32_t* groups;  // what the groups before each have, and last where each digit's places begin; null where counts are not scanned
   uint32_t t, v, blocks;
   int shift;
   uint32_t mask;
@@ -112,7 +118,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_count(const SortArgs a) {
     if (i < a.t) atomicAdd(&count[(key_at<I, FIRST>(a, i) >> a.shift) & a.mask], 1u);
   }
   __syncthreads();
-  a.counts[blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
+  a.counts[(int64_t)blockIdx.x * DIGITS + threadIdx.x] = count[threadIdx.x];
 }
 
 // Exclusive sum over the 512 threads of a workgroup.
@@ -129,6 +135,34 @@ __device__ __forceinline__ uint32_t exclusive_sum(uint32_t x, uint32_t* scratch 
   uint32_t before = 0;
   for (int w = 0; w < wave; ++w) before += scratch[w];
   return before + sum - x;
+}
+
+// A column of `rows` counts into running sums (what the rows before each have); what all of them have.  Thread = digit, 32 loads under way at a time.
+__device__ __forceinline__ uint32_t scan_column(uint32_t* counts, uint32_t rows) {
+  uint32_t sum = 0;
+  for (uint32_t b = 0; b < rows; b += 32) {
+    uint32_t c[32];
+#pragma unroll
+    for (int q = 0; q < 32; ++q) c[q] = b + q < rows ? counts[(int64_t)(b + q) * DIGITS + threadIdx.x] : 0;
+#pragma unroll
+    for (int q = 0; q < 32; ++q) {
+      if (b + q < rows) counts[(int64_t)(b + q) * DIGITS + threadIdx.x] = sum;
+      sum += c[q];
+    }
+  }
+  return sum;
+}
+
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_scan(const SortArgs a) {
+  const uint32_t first = blockIdx.x * SCAN_BLOCKS;
+  a.groups[(int64_t)blockIdx.x * DIGITS + threadIdx.x] = scan_column(a.counts + (int64_t)first * DIGITS, min((uint32_t)SCAN_BLOCKS, a.blocks - first));
+}
+
+// One workgroup: the groups' sums, and where each digit's places begin.
+__global__ __launch_bounds__(SORT_THREADS) void k_sort_scan_groups(const SortArgs a, const uint32_t groups) {
+  __shared__ uint32_t scratch[SORT_THREADS / 64];
+  const uint32_t all = scan_column(a.groups, groups);
+  a.groups[(int64_t)groups * DIGITS + threadIdx.x] = exclusive_sum(all, scratch);
 }
 
 template <typename I, bool FIRST>
@@ -171,18 +205,25 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(const SortArgs a)
   }
   __syncthreads();
   // thread = digit: its places in all blocks and in those before this one, and in the block's wavefronts
-  uint32_t all = 0, before = 0;
-  for (uint32_t b = 0; b < a.blocks; b += 32) {  // (thirty-two loads under way at a time)
-    uint32_t c[32];
+  uint32_t to;
+  if (a.groups) {
+    const uint32_t groups = (a.blocks + SCAN_BLOCKS - 1) / SCAN_BLOCKS;
+    to = a.counts[(int64_t)blockIdx.x * DIGITS + threadIdx.x] + a.groups[(int64_t)(blockIdx.x / SCAN_BLOCKS) * DIGITS + threadIdx.x] +
+         a.groups[(int64_t)groups * DIGITS + threadIdx.x];
+  } else {
+    uint32_t all = 0, before = 0;
+    for (uint32_t b = 0; b < a.blocks; b += 32) {  // (thirty-two loads under way at a time)
+      uint32_t c[32];
 #pragma unroll
-    for (int q = 0; q < 32; ++q) c[q] = b + q < a.blocks ? a.counts[(b + q) * DIGITS + threadIdx.x] : 0;
+      for (int q = 0; q < 32; ++q) c[q] = b + q < a.blocks ? a.counts[(b + q) * DIGITS + threadIdx.x] : 0;
 #pragma unroll
-    for (int q = 0; q < 32; ++q) {
-      all += c[q];
-      before += b + q < blockIdx.x ? c[q] : 0;
+      for (int q = 0; q < 32; ++q) {
+        all += c[q];
+        before += b + q < blockIdx.x ? c[q] : 0;
+      }
     }
+    to = exclusive_sum(all, scratch) + before;
   }
-  uint32_t to = exclusive_sum(all, scratch) + before;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) {
     const uint32_t c = at[w][threadIdx.x];
@@ -629,7 +670,8 @@ int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, i
   while ((v >> bits) != 0) ++bits;  // of v, the key of no token
   const int passes = (bits + DIGIT_BITS - 1) / DIGIT_BITS, digit = (bits + passes - 1) / passes;
   const int64_t blocks = (t + SORT_BLOCK - 1) / SORT_BLOCK, pieces = (t + CHUNK - 1) / CHUNK, width = up(d, 8);
-  const int64_t list = up(8 * t, 256), counts = blocks * DIGITS * 4;
+  const int64_t list = up(8 * t, 256), groups = blocks >= SCAN_FROM ? (blocks + SCAN_BLOCKS - 1) / SCAN_BLOCKS : 0;
+  const int64_t counts = blocks * DIGITS * 4, group_counts = groups ? (groups + 1) * DIGITS * 4 : 0;
   GradArgs g;
   memset(&g, 0, sizeof(g));
   g.dY = dY, g.ldy = ldy, g.d = d, g.t = (uint32_t)t, g.v = (uint32_t)v, g.scale = scale, g.G = G, g.ldg = ldg;
@@ -660,24 +702,32 @@ int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, i
     EJ_TRY(hipGetLastError());
     return EJOIN_OK;
   }
-  EJ_RC(ensure_embed(ctx, 2 * list + counts + pieces * 2 * width * 4));
+  EJ_RC(ensure_embed(ctx, 2 * list + counts + group_counts + pieces * 2 * width * 4));
   uint2* lists[2] = {reinterpret_cast<uint2*>(ctx->embed), reinterpret_cast<uint2*>(ctx->embed + list)};
-  g.parts = reinterpret_cast<float*>(ctx->embed + 2 * list + counts);
+  g.parts = reinterpret_cast<float*>(ctx->embed + 2 * list + counts + group_counts);
   SortArgs s;
   memset(&s, 0, sizeof(s));
   s.tokens = tokens, s.counts = reinterpret_cast<uint32_t*>(ctx->embed + 2 * list), s.t = (uint32_t)t, s.v = (uint32_t)v, s.blocks = (uint32_t)blocks;
+  s.groups = groups ? s.counts + blocks * DIGITS : nullptr;
   s.mask = (1u << digit) - 1, s.status = ctx->token_status;
   for (int pass = 0; pass < passes; ++pass) {
     s.items = lists[pass & 1], s.items_out = lists[1 - (pass & 1)];
     s.shift = pass * digit;
     const dim3 grid((unsigned)blocks), block(SORT_THREADS);
+    auto scan = [&] {
+      if (!groups) return;
+      hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)groups), block, 0, st, s);
+      hipLaunchKernelGGL(k_sort_scan_groups, dim3(1), block, 0, st, s, (uint32_t)groups);
+    };
     if (pass == 0) {
       with_index(token_type, [&](auto i) {
         hipLaunchKernelGGL((k_sort_count<decltype(i), true>), grid, block, 0, st, s);
+        scan();
         hipLaunchKernelGGL((k_sort_scatter<decltype(i), true>), grid, block, 0, st, s);
       });
     } else {
       hipLaunchKernelGGL((k_sort_count<int32_t, false>), grid, block, 0, st, s);
+      scan();
       hipLaunchKernelGGL((k_sort_scatter<int32_t, false>), grid, block, 0, st, s);
     }
     EJ_TRY(hipGetLastError());
