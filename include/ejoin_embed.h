@@ -36,8 +36,8 @@ int ejoin_embed_reserve(ejoin_ctx* ctx, int64_t bytes);
  * x[k] * 2^-e, 2^e the least power of two that brings the block's largest finite magnitude into the format's range (448 for
  * E4M3, 57344 for E5M2); e + 127 is the block's scale byte, cut off at 0 (and 127 for a block of zeros).  So no value
  * saturates, and multiplying by a scale never rounds.  NaN stays NaN; an infinity becomes NaN in E4M3 and stays one in E5M2.
- *   values  n rows of roundup(d, 128) bytes, row stride ld (a multiple of 128), 128-byte aligned; coordinates d and up are zero
- *   scales  n rows of roundup(ceil(d / 128), 4) bytes, row stride ld_scales (a multiple of 4), 4-byte aligned;
+ *   values  n rows of roundup(d, 128) bytes, row stride ld (a multiple of 128, at most 2^23), 128-byte aligned; coordinates d and up are zero
+ *   scales  n rows of roundup(ceil(d / 128), 4) bytes, row stride ld_scales (a multiple of 4, at most 2^24), 4-byte aligned;
  *           bytes past the last block hold 127 */
 #define EJOIN_E4M3 0
 #define EJOIN_E5M2 1

@@ -1047,12 +1047,13 @@ __global__ __launch_bounds__(256) void k_add_parts(const ProductArgs a, const in
 
 // ------------------------------------------------------------------------------------------ host side
 constexpr int64_t MOST = 1ll << 23;  // coordinates of a row: 256 rows of them are within 31 bits of their first
+constexpr int64_t MOST_SCALES = 1ll << 24;  // bytes between rows of scales: those of 256 rows are within 32 bits of their first
 
 bool bad_rows(const ejoin_f8_rows* r, int64_t most_rows) {
   if (!r || !r->values || !r->scales || (r->format != EJOIN_E4M3 && r->format != EJOIN_E5M2)) return true;
   if (r->n < 1 || r->n >= most_rows || r->d < 1 || r->d >= MOST) return true;
   const int64_t width = up(r->d, BLOCK), scales = up(f8_blocks(r->d), 4);
-  if (r->ld < width || r->ld % BLOCK != 0 || r->ld > MOST || r->ld_scales < scales || r->ld_scales % 4 != 0) return true;
+  if (r->ld < width || r->ld % BLOCK != 0 || r->ld > MOST || r->ld_scales < scales || r->ld_scales % 4 != 0 || r->ld_scales > MOST_SCALES) return true;
   return (reinterpret_cast<uintptr_t>(r->values) & 127) != 0 || (reinterpret_cast<uintptr_t>(r->scales) & 3) != 0;
 }
 
