@@ -22,6 +22,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (not part 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _INDEX_TYPES = {torch.int32: 0, torch.int64: 1}
 _F8_FORMATS = {"e4m3": 0, "e5m2": 1}
+# (bytes may come as whole numbers, or as torch's own type for what they stand for)
+_F8_VALUES = {"e4m3": (torch.uint8, torch.int8, torch.float8_e4m3fn), "e5m2": (torch.uint8, torch.int8, torch.float8_e5m2)}
+_F8_SCALES = (torch.uint8, torch.float8_e8m0fnu)
 F8_BLOCK = 128  # coordinates that share a scale
 
 
@@ -37,8 +40,8 @@ class _F8RowsC(C.Structure):  # ejoin_f8_rows
 class F8Rows:
     """Rows of d coordinates in 8-bit floating point ("e4m3" or "e5m2") with a power-of-two scale for each block of 128 (ejoin_f8_rows).
 
-    values  (n, roundup(d, 128)) device tensor of one-byte elements, zero from column d on
-    scales  (n, roundup(ceil(d / 128), 4)) uint8 device tensor of exponents + 127"""
+    values  (n, roundup(d, 128)) device tensor of bytes (uint8, int8, or torch's type of the format), zero from column d on
+    scales  (n, roundup(ceil(d / 128), 4)) device tensor of exponents + 127 (uint8 or float8_e8m0fnu)"""
 
     def __init__(self, values: torch.Tensor, scales: torch.Tensor, d: int, format: str = "e4m3"):
         code = _F8_FORMATS.get(format)
@@ -46,16 +49,16 @@ class F8Rows:
             raise EJoinError('format must be "e4m3" or "e5m2"')
         self.values, self.scales, self.d, self.format = values, scales, int(d), format
         blocks = (self.d + F8_BLOCK - 1) // F8_BLOCK
-        self.n, ld = self._rows(values, blocks * F8_BLOCK, "values")
-        n, ld_scales = self._rows(scales, (blocks + 3) // 4 * 4, "scales")
+        self.n, ld = self._rows(values, blocks * F8_BLOCK, "values", _F8_VALUES[format])
+        n, ld_scales = self._rows(scales, (blocks + 3) // 4 * 4, "scales", _F8_SCALES)
         if n != self.n or values.get_device() != scales.get_device():
             raise EJoinError("values and scales must be of the same rows, on one device")
         self._c = _F8RowsC(values.data_ptr(), scales.data_ptr(), ld, ld_scales, n, self.d, code)
 
     @staticmethod
-    def _rows(x: torch.Tensor, width: int, what: str):
-        if x.dim() != 2 or x.element_size() != 1 or x.get_device() < 0 or x.shape[1] < width or x.stride(1) != 1:
-            raise EJoinError(f"{what} must be a 2-D device tensor of one-byte elements with contiguous rows of at least {width}")
+    def _rows(x: torch.Tensor, width: int, what: str, types: tuple):
+        if x.dim() != 2 or x.dtype not in types or x.get_device() < 0 or x.shape[1] < width or x.stride(1) != 1:
+            raise EJoinError(f"{what} must be a 2-D device tensor of {' or '.join(map(str, types))} with contiguous rows of at least {width}")
         n = x.shape[0]
         return n, x.stride(0) if n > 1 else x.shape[1]
 
@@ -69,7 +72,7 @@ class F8Rows:
         """What the rows stand for: (n, d) float32 (plain torch, for inspection)."""
         blocks = (self.d + F8_BLOCK - 1) // F8_BLOCK
         values = self.values[:, :blocks * F8_BLOCK].contiguous().view(torch.float8_e4m3fn if self.format == "e4m3" else torch.float8_e5m2)
-        scales = torch.exp2(self.scales[:, :blocks].float() - 127.0)
+        scales = torch.exp2(self.scales.view(torch.uint8)[:, :blocks].float() - 127.0)
         return (values.float().view(self.n, blocks, F8_BLOCK) * scales[:, :, None]).view(self.n, blocks * F8_BLOCK)[:, :self.d]
 
 

@@ -34,3 +34,19 @@ def test_scales_far_apart(ej):
         with pytest.raises(pkg.EJoinError):
             call()
     torch.cuda.synchronize()
+
+
+def test_rows_of_another_format_are_refused(ej):
+    x = torch.randn((70, 200), device="cuda")
+    types = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+    for form, other in (("e4m3", "e5m2"), ("e5m2", "e4m3")):
+        q = ej.quantize_f8(x, form)
+        same = pkg.F8Rows(q.values.view(types[form]), q.scales, 200, form)
+        assert torch.equal(same.float(), q.float()) and torch.equal(ej.product_f8(same, q), ej.product_f8(q, q))
+        assert torch.equal(pkg.F8Rows(q.values, q.scales.view(torch.float8_e8m0fnu), 200, form).float(), q.float())
+        for dtype in (types[other], torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.float8_e8m0fnu, torch.bool):
+            with pytest.raises(pkg.EJoinError):
+                pkg.F8Rows(q.values.view(dtype), q.scales, 200, form)
+        for dtype in (torch.float8_e4m3fn, torch.int8, torch.bool):
+            with pytest.raises(pkg.EJoinError):
+                pkg.F8Rows(q.values, q.scales.view(dtype), 200, form)
