@@ -53,7 +53,7 @@ typedef struct {
 
 /* X (n x d, row stride ldx >= d) into 8-bit rows: `rows` takes X's own rows (rows->n = n, rows->d = d), `columns` those
  * of X transposed (columns->n = d, columns->d = n); either may be NULL.  Both are host structs whose format,
- * pointers and strides the caller fills in; with both, X is read once.  1 <= n, d < 2^23. */
+ * pointers and strides the caller fills in; with both, X is read once.  1 <= n, d < 2^23; rows alone may be up to 2^31 - 1. */
 int ejoin_f8_quantize(ejoin_ctx* ctx, const void* X, int32_t type, int64_t n, int64_t d, int64_t ldx, const ejoin_f8_rows* rows,
                       const ejoin_f8_rows* columns, void* stream);
 

@@ -91,6 +91,9 @@ inline bool bad_type(int32_t type) { return type != EJOIN_F32 && type != EJOIN_F
 inline int64_t size_of(int32_t type) { return type == EJOIN_F32 ? 4 : 2; }
 inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+// A launch has fewer than 2^32 threads: so many workgroups, of 1,024 threads at most, are one launch's.
+constexpr int64_t MOST_GROUPS = 1ll << 21;
+
 // f(T()) with the type that `type` names.
 template <typename F>
 auto with_type(int32_t type, F f) {

@@ -58,6 +58,7 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
 struct QuantArgs {
   const void* X;
   int64_t n, d, ldx;
+  int64_t first;    // row that the launch begins with (k_quantize_rows)
   uint32_t blocks;  // of a row
   uint8_t* rows;
   uint8_t* row_scales;
@@ -185,7 +186,7 @@ constexpr int QUANT_ROWS = 4;
 template <typename T, int FMT>
 __global__ __launch_bounds__(256) void k_quantize_rows(const QuantArgs a) {
   const uint32_t group = blockIdx.x / a.blocks, block = blockIdx.x - group * a.blocks, lane = threadIdx.x & 15;
-  const int64_t row0 = (int64_t)group * (16 * QUANT_ROWS) + (threadIdx.x >> 4), at = (int64_t)block * BLOCK + lane * 8;
+  const int64_t row0 = a.first + (int64_t)group * (16 * QUANT_ROWS) + (threadIdx.x >> 4), at = (int64_t)block * BLOCK + lane * 8;
   Octet<T> x[QUANT_ROWS];
 #pragma unroll
   for (int i = 0; i < QUANT_ROWS; ++i) {
@@ -1069,15 +1070,24 @@ int launch_quantize(ejoin_ctx* ctx, const void* X, int32_t type, int64_t n, int6
   if (rows) a.rows = rows->values, a.row_scales = rows->scales, a.ld_rows = rows->ld, a.ld_row_scales = rows->ld_scales;
   if (columns) a.cols = columns->values, a.col_scales = columns->scales, a.ld_cols = columns->ld, a.ld_col_scales = columns->ld_scales;
   const bool e4m3 = (rows ? rows : columns)->format == EJOIN_E4M3;
-  const int64_t groups = (columns ? f8_blocks(n) : (n + 16 * QUANT_ROWS - 1) / (16 * QUANT_ROWS)) * a.blocks;
-  if (groups > 0x7FFFFFFFll) return EJOIN_EUNSUPPORTED;
+  const int64_t tiles = f8_blocks(n) * a.blocks;
+  if (columns && tiles > 4 * MOST_GROUPS) return EJOIN_EUNSUPPORTED;  // (of 256 threads: X would be 2^37 values)
   with_type(type, [&](auto t) {
     typedef decltype(t) T;
     void (*kernel)(QuantArgs) = nullptr;
     if (!columns) kernel = e4m3 ? &k_quantize_rows<T, EJOIN_E4M3> : &k_quantize_rows<T, EJOIN_E5M2>;
     else if (!rows) kernel = e4m3 ? &k_quantize_tile<T, EJOIN_E4M3, false> : &k_quantize_tile<T, EJOIN_E5M2, false>;
     else kernel = e4m3 ? &k_quantize_tile<T, EJOIN_E4M3, true> : &k_quantize_tile<T, EJOIN_E5M2, true>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, st, a);
+    if (columns) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(256), 0, st, a);
+      return;
+    }
+    constexpr int64_t ROWS = 16 * QUANT_ROWS;  // of a workgroup
+    const int64_t most = MOST_GROUPS / a.blocks * ROWS;
+    for (a.first = 0; a.first < n; a.first += most) {
+      const int64_t here = n - a.first < most ? n - a.first : most;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((here + ROWS - 1) / ROWS * a.blocks)), dim3(256), 0, st, a);
+    }
   });
   EJ_TRY(hipGetLastError());
   return EJOIN_OK;
@@ -1222,8 +1232,8 @@ int ejoin_embed_reserve(ejoin_ctx* ctx, int64_t bytes) {
 
 int ejoin_f8_quantize(ejoin_ctx* ctx, const void* X, int32_t type, int64_t n, int64_t d, int64_t ldx, const ejoin_f8_rows* rows,
                       const ejoin_f8_rows* columns, void* stream) {
-  if (!ctx || !X || bad_type(type) || n < 1 || n >= MOST || d < 1 || d >= MOST || ldx < d || (!rows && !columns)) return EJOIN_EINVAL;
-  if (rows && (bad_rows(rows, MOST) || rows->n != n || rows->d != d)) return EJOIN_EINVAL;
+  if (!ctx || !X || bad_type(type) || n < 1 || n >= (columns ? MOST : 1ll << 31) || d < 1 || d >= MOST || ldx < d || (!rows && !columns)) return EJOIN_EINVAL;
+  if (rows && (bad_rows(rows, 1ll << 31) || rows->n != n || rows->d != d)) return EJOIN_EINVAL;
   if (columns && (bad_rows(columns, MOST) || columns->n != d || columns->d != n)) return EJOIN_EINVAL;
   if (rows && columns && rows->format != columns->format) return EJOIN_EINVAL;
   DeviceGuard guard(ctx->device);

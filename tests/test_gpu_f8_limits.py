@@ -50,3 +50,30 @@ def test_rows_of_another_format_are_refused(ej):
         for dtype in (torch.float8_e4m3fn, torch.int8, torch.bool):
             with pytest.raises(pkg.EJoinError):
                 pkg.F8Rows(q.values, q.scales.view(dtype), 200, form)
+
+
+@pytest.mark.parametrize("n,d,dtype", [((1 << 23) + 77, 3, torch.float32), ((1 << 23) - 1, 129, torch.float16), ((1 << 28) + 5, 1, torch.bfloat16)])
+def test_rows_in_8_bits_past_2_to_the_23(ej, n, d, dtype):
+    """A row's bytes depend on that row alone: those of a large matrix are those of its pieces."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.randn((n, d), generator=gen, device="cuda", dtype=torch.float16 if n > 1 << 27 else torch.float32).to(dtype)
+    q = ej.quantize_f8(x)
+    for at in (0, 1 << 22, n // 2 + 1, n - 1000):
+        piece = ej.quantize_f8(x[at:at + 1000])
+        assert torch.equal(q.values[at:at + 1000], piece.values) and torch.equal(q.scales[at:at + 1000], piece.scales)
+    if n > 1 << 27:
+        at = (1 << 21) * 64 * 2  # (a border between launches)
+        piece = ej.quantize_f8(x[at - 70:])
+        assert torch.equal(q.values[at - 70:], piece.values) and torch.equal(q.scales[at - 70:], piece.scales)
+    del x, q
+    torch.cuda.empty_cache()
+
+
+def test_columns_of_so_many_rows_are_refused(ej):
+    """Along the columns a row of the result is as long as X has rows."""
+    x = torch.zeros((1 << 23, 2), dtype=torch.float16, device="cuda")
+    with pytest.raises(pkg.EJoinError):
+        ej.quantize_f8(x, columns=True)
+    with pytest.raises(pkg.EJoinError):
+        ej.quantize_f8_both(x)
+    assert ej.quantize_f8(x[:-1], columns=True).n == 2
