@@ -39,6 +39,7 @@ __device__ __forceinline__ float lse_of(Stats s, float inv_t) { return nothing(s
 struct DistillArgs {
   const void* Z;
   int64_t t, v, ldz;
+  int64_t first;  // row that the launch begins with (k_distill_row)
   const void* ids;
   int32_t id_type;
   const float* teacher;
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREA
   __shared__ List list;
   __shared__ Stats wave_stats[THREADS / 64];
   __shared__ float shared_list_top;
-  const int64_t row = blockIdx.x;
+  const int64_t row = a.first + blockIdx.x;
   const T* z = static_cast<const T*>(a.Z) + row * a.ldz;
   const uint32_t v = (uint32_t)a.v, whole = v & ~7u, mine = threadIdx.x * 8;
   Words<T> x[PIECES];
@@ -454,11 +455,14 @@ int launch_distill(ejoin_ctx* ctx, DistillArgs& a, int32_t ztype, hipStream_t st
     int threads;
     const DistillKernel kernel = row_kernel<T, FORWARD, GRAD>(a.v, threads);
     if (kernel && !few_long<FORWARD && GRAD>(ctx, a.t, a.v)) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)a.t), dim3(threads), 0, st, a);
+      in_launches(a.t, [&](int64_t first, unsigned rows) {
+        a.first = first;
+        hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, st, a);
+      });
       return;
     }
     split_rows(ctx, a);
-    if (a.t * a.splits > 0x7FFFFFFFll) {
+    if (a.t * a.splits > MOST_GROUPS) {  // (more than 2^21 rows of more than 32,768 scores)
       rc = EJOIN_EUNSUPPORTED;
       return;
     }

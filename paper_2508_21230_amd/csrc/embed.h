@@ -93,6 +93,11 @@ inline int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // A launch has fewer than 2^32 threads: so many workgroups, of 1,024 threads at most, are one launch's.
 constexpr int64_t MOST_GROUPS = 1ll << 21;
+// launch(first, groups) for `groups` workgroups in as many launches as that takes.
+template <typename F>
+void in_launches(int64_t groups, F launch) {
+  for (int64_t first = 0; first < groups; first += MOST_GROUPS) launch(first, (unsigned)(groups - first < MOST_GROUPS ? groups - first : MOST_GROUPS));
+}
 
 // f(T()) with the type that `type` names.
 template <typename F>

@@ -423,13 +423,13 @@ __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
 constexpr int JOIN_THREADS = 512;
 constexpr int JOIN_PIECES = 8;
 template <typename O>
-__global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(const GradArgs a) {
+__global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(const GradArgs a, const uint32_t first_block) {
   __shared__ float sums[JOIN_THREADS * 8];
   __shared__ uint64_t found;
   const uint32_t lane = threadIdx.x & ((1u << a.lanes_log2) - 1), mine = threadIdx.x >> a.lanes_log2, groups = JOIN_THREADS >> a.lanes_log2;
   const uint32_t pieces = (uint32_t)(((uint64_t)a.t + CHUNK - 1) / CHUNK);
   if (threadIdx.x < 64) {
-    const uint32_t group = blockIdx.x * JOIN_PIECES + threadIdx.x, p0 = group * CHUNK, p1 = p0 + CHUNK;
+    const uint32_t group = (first_block + blockIdx.x) * JOIN_PIECES + threadIdx.x, p0 = group * CHUNK, p1 = p0 + CHUNK;
     bool begins = threadIdx.x < JOIN_PIECES && (uint64_t)group + 2 < pieces;
     if (begins) {
       const uint32_t row = a.items[p1 - 1].x, third = a.items[p1 + CHUNK].x, first = a.items[p0].x, before = p0 ? a.items[p0 - 1].x : 0xFFFFFFFFu;
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(const GradArgs a) {
   }
   __syncthreads();
   for (uint64_t left = found; left; left &= left - 1) {
-    const uint32_t group = blockIdx.x * JOIN_PIECES + __builtin_ctzll(left), row = a.items[group * CHUNK + CHUNK - 1].x;
+    const uint32_t group = (first_block + blockIdx.x) * JOIN_PIECES + __builtin_ctzll(left), row = a.items[group * CHUNK + CHUNK - 1].x;
     // parts: of this piece, and of those after it whose first key is the row's (a thread looks at each: a search would wait for the memory some twenty times)
     uint32_t number = 1;
     for (int more = JOIN_THREADS; more == JOIN_THREADS; number += more) {
@@ -496,7 +496,8 @@ constexpr int SMALL_PLACES = 8192;  // at most
 struct SmallArgs {
   GradArgs g;
   const void* tokens;
-  uint32_t rows;  // of a workgroup
+  uint32_t rows;   // of a workgroup
+  uint32_t first;  // workgroup that the launch begins with
 };
 
 template <typename T, typename O, typename I, int PLACES, int THREADS>
@@ -508,7 +509,7 @@ __global__ __launch_bounds__(THREADS) void k_grad_small(const SmallArgs s) {
   __shared__ float sums[THREADS * 8];
   const GradArgs& a = s.g;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t row0 = blockIdx.x * s.rows, rows = min(s.rows, a.v - row0);
+  const uint32_t row0 = (s.first + blockIdx.x) * s.rows, rows = min(s.rows, a.v - row0);
   if (threadIdx.x < SMALL_ROWS) cursor[threadIdx.x] = 0;
   // each wavefront: its share of the tokens, all under way together
   constexpr int TOKENS = PLACES / THREADS;  // of a lane
@@ -636,7 +637,7 @@ int ejoin_lookup(ejoin_ctx* ctx, const void* table, int32_t type, int64_t v, int
   if (!guard.ok) return EJOIN_EHIP;
   LookupArgs a{table, v, ldt, d, tokens, t, scale, Y, ldy, (uint32_t)(up(d, 64) / 8), ctx->token_status};
   const int64_t units = t * a.chunks, groups = (units + 256 * LOOKUP_PIECES - 1) / (256 * LOOKUP_PIECES);
-  if (groups > 0x7FFFFFFFll) return EJOIN_EUNSUPPORTED;
+  if (groups >= 1ll << 24) return EJOIN_EUNSUPPORTED;  // (of 256 threads: Y would be 2^37 values)
   const bool wide = units + 256 * LOOKUP_PIECES >= (1ll << 32);
   // 16-bit results that the memory-side cache does not hold, 307 MB of 400,003 rows of 384, tokens evenly spread over 1,000,000 FP32 rows: 166 us through the
   // caches, 142 past them.  (FP32 ones, whose pieces are two stores, are the slower for it: 102 MB 28 and 40 us.)
@@ -684,18 +685,21 @@ int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, i
     // some 1,024 workgroups, where there are rows enough
     int64_t rows = (v + 1023) / 1024;
     rows = rows < 8 ? 8 : (rows < SMALL_ROWS ? rows : SMALL_ROWS);
-    const SmallArgs a{g, tokens, (uint32_t)rows};
+    SmallArgs a{g, tokens, (uint32_t)rows, 0};
     with_type(gtype, [&](auto o) {
       with_type(type, [&](auto x) {
         with_index(token_type, [&](auto i) {
           typedef decltype(x) X;
           typedef decltype(o) O;
           typedef decltype(i) I;
-          const dim3 grid((unsigned)((v + rows - 1) / rows));
           // (room for no more places than there may be: 1,000 tokens of 50,000 rows of 300 32 us with room for 1,024, 49 with room for 8,192)
-          if (t <= 1024) hipLaunchKernelGGL((k_grad_small<X, O, I, 1024, 256>), grid, dim3(256), 0, st, a);
-          else if (t <= 4096) hipLaunchKernelGGL((k_grad_small<X, O, I, 4096, 512>), grid, dim3(512), 0, st, a);
-          else hipLaunchKernelGGL((k_grad_small<X, O, I, SMALL_PLACES, 512>), grid, dim3(512), 0, st, a);
+          void (*kernel)(SmallArgs) = t <= 1024   ? &k_grad_small<X, O, I, 1024, 256>
+                                      : t <= 4096 ? &k_grad_small<X, O, I, 4096, 512>
+                                                  : &k_grad_small<X, O, I, SMALL_PLACES, 512>;
+          in_launches((v + rows - 1) / rows, [&](int64_t first, unsigned groups) {
+            a.first = (uint32_t)first;
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(t <= 1024 ? 256 : 512), 0, st, a);
+          });
         });
       });
     });
@@ -735,11 +739,13 @@ int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, i
   }
   g.sum_groups = (uint32_t)(((pieces << g.lanes_log2) + 255) / 256);
   g.zero_rows = 256;
+  // (one launch: 2^23 workgroups of zeros at most, and rows of 64 columns, the most that 2^31 places may have, take 2^21 of sums)
   const dim3 grid((unsigned)(g.sum_groups + (v + g.zero_rows - 1) / g.zero_rows));
   with_type(gtype, [&](auto o) {
     typedef decltype(o) O;
     with_type(type, [&](auto x) { hipLaunchKernelGGL((k_grad_sum<decltype(x), O>), grid, dim3(256), 0, st, g); });
-    hipLaunchKernelGGL(k_grad_join<O>, dim3((unsigned)((pieces + JOIN_PIECES - 1) / JOIN_PIECES)), dim3(JOIN_THREADS), 0, st, g);
+    in_launches((pieces + JOIN_PIECES - 1) / JOIN_PIECES,
+                [&](int64_t first, unsigned groups) { hipLaunchKernelGGL(k_grad_join<O>, dim3(groups), dim3(JOIN_THREADS), 0, st, g, (uint32_t)first); });
   });
   EJ_TRY(hipGetLastError());
   return EJOIN_OK;
