@@ -661,7 +661,7 @@ int ejoin_lookup(ejoin_ctx* ctx, const void* table, int32_t type, int64_t v, int
 
 int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, int32_t d, int64_t ldy, const void* tokens, int32_t token_type, int64_t v,
                       float scale, void* G, int32_t gtype, int64_t ldg, void* stream) {
-  if (!ctx || !G || bad_type(type) || bad_type(gtype) || v < 1 || v >= (1ll << 31) - 1 || d < 1 || d > 65536 || ldg < d) return EJOIN_EINVAL;
+  if (!ctx || !G || bad_type(type) || bad_type(gtype) || v < 1 || v >= (1ll << 31) || d < 1 || d > 65536 || ldg < d) return EJOIN_EINVAL;
   if (t < 0 || t >= (1ll << 31) || !isfinite(scale) || ldy < d) return EJOIN_EINVAL;
   if (t > 0 && (!dY || bad_tokens(tokens, token_type))) return EJOIN_EINVAL;
   DeviceGuard guard(ctx->device);

@@ -39,7 +39,7 @@ def test_loss_of_many_rows(ej, t, dtype):
 
 
 @pytest.mark.parametrize("t", [5, 3000, 9000])
-@pytest.mark.parametrize("v", [(1 << 31) - 2, (1 << 28) + 65])
+@pytest.mark.parametrize("v", [(1 << 31) - 1, (1 << 31) - 2, (1 << 28) + 65])
 def test_largest_tables(ej, t, v):
     gen = torch.Generator(device="cuda").manual_seed(t)
     tokens = torch.randint(v, (t,), generator=gen, device="cuda")
