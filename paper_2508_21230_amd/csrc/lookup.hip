@@ -648,9 +648,12 @@ int ejoin_lookup(ejoin_ctx* ctx, const void* table, int32_t type, int64_t v, int
         typedef decltype(x) X;
         typedef decltype(y) Y;
         typedef decltype(i) I;
-        void (*kernel)(LookupArgs) = wide ? k_lookup<X, Y, I, true, false> : k_lookup<X, Y, I, false, false>;
-        if constexpr (sizeof(Y) == 2)
-          if (passing) kernel = wide ? k_lookup<X, Y, I, true, true> : k_lookup<X, Y, I, false, true>;
+        void (*kernel)(LookupArgs) = k_lookup<X, Y, I, false, false>;
+        if constexpr (sizeof(Y) == 2) {
+          if (passing) kernel = wide ? k_lookup<X, Y, I, true, true> : k_lookup<X, Y, I, false, true>;  // (wide ones are 68 GB)
+        } else {
+          if (wide) kernel = k_lookup<X, Y, I, true, false>;
+        }
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, static_cast<hipStream_t>(stream), a);
       });
     });
