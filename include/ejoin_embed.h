@@ -8,7 +8,9 @@
  *   - Matrices are row-major with a row stride in elements >= their width; rows need no alignment and no padding
  *     except where a call says so.
  *   - A call that needs device memory to work in takes it from the context, which grows it on demand (the growth
- *     waits for the device, as that of the joins' workspace does) or ahead of time (ejoin_embed_reserve).
+ *     waits for the device, as that of the joins' workspace does) or ahead of time (ejoin_embed_reserve).  Where a
+ *     call is to be captured into a graph the memory has to be there before.  A graph works in the memory that it was captured
+ *     with: the context keeps it until it is destroyed, also when it has grown since, and a replay is a call on the context like any other.
  *   - Sizes of zero rows are allowed where noted, and enqueue nothing.
  *   - Results are the same bits from call to call: no sum is taken in an order that depends on timing.
  */

@@ -45,6 +45,9 @@ struct ejoin_ctx {
   // ejoin_embed.h: memory its calls work in, grown on demand, and the device word in which they leave what was wrong with tokens
   unsigned char* embed;
   int64_t embed_bytes;
+  bool embed_captured;      // a call that works in it was recorded into a graph: it stays where it is until the context ends
+  unsigned char** retired;  // such memory that was grown out of
+  int64_t num_retired;
   uint32_t* token_status;  // word EJ_TOKEN_STATUS of the context's own status block
   uint32_t* tickets;       // device: EJ_TICKETS counters, all zero between calls
   char hip_error[256];

@@ -469,7 +469,7 @@ int launch_distill(ejoin_ctx* ctx, DistillArgs& a, int32_t ztype, hipStream_t st
     const dim3 grid((unsigned)(a.t * a.splits));
     if (FORWARD) {
       const int64_t parts = up(a.t * a.splits * (int64_t)sizeof(Stats), 256);
-      rc = ensure_embed(ctx, parts + (GRAD ? a.t * (int64_t)sizeof(Stats) : 0));
+      rc = ensure_embed(ctx, parts + (GRAD ? a.t * (int64_t)sizeof(Stats) : 0), st);
       if (rc != EJOIN_OK) return;
       a.parts = reinterpret_cast<Stats*>(ctx->embed);
       a.tickets = ctx->tickets;

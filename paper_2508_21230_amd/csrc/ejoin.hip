@@ -8,6 +8,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 #include <math.h>
 #include <new>
@@ -3913,6 +3914,8 @@ int ejoin_destroy(ejoin_ctx* ctx) {
   if (ctx->ws.s) (void)hipFree(ctx->ws.s);
   if (ctx->ws.Xp) (void)hipFree(ctx->ws.Xp);
   if (ctx->embed) (void)hipFree(ctx->embed);
+  for (int64_t i = 0; i < ctx->num_retired; ++i) (void)hipFree(ctx->retired[i]);
+  free(ctx->retired);
   if (ctx->tickets) (void)hipFree(ctx->tickets);
   for (int i = 0; i < 4; ++i)
     if (ctx->ev[i]) (void)hipEventDestroy(ctx->ev[i]);

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include "context.h"
@@ -109,15 +110,22 @@ auto with_type(int32_t type, F f) {
   }
 }
 
-// The context's memory for these calls, at least `bytes` of it.  Growing frees the old, which first waits for the device to be idle.
+// The context's memory for these calls, at least `bytes` of it.  Growing frees the old, which first waits for the device to be idle; but memory that a
+// captured graph may come back to is kept, and nothing is waited for then.
 inline int ensure_embed(ejoin_ctx* ctx, int64_t bytes) {
   if (bytes <= ctx->embed_bytes) return EJOIN_OK;
-  if (ctx->embed) {
+  if (ctx->embed && ctx->embed_captured) {
+    unsigned char** more = static_cast<unsigned char**>(realloc(ctx->retired, (size_t)(ctx->num_retired + 1) * sizeof(*more)));
+    if (!more) return EJOIN_ENOMEM;
+    ctx->retired = more;
+    ctx->retired[ctx->num_retired++] = ctx->embed;
+    ctx->embed_captured = false;
+  } else if (ctx->embed) {
     EJ_TRY(hipDeviceSynchronize());
     EJ_TRY(hipFree(ctx->embed));
-    ctx->embed = nullptr;
-    ctx->embed_bytes = 0;
   }
+  ctx->embed = nullptr;
+  ctx->embed_bytes = 0;
   const hipError_t e = hipMalloc(reinterpret_cast<void**>(&ctx->embed), (size_t)bytes);
   if (e != hipSuccess) {
     (void)hipGetLastError();
@@ -126,6 +134,15 @@ inline int ensure_embed(ejoin_ctx* ctx, int64_t bytes) {
     return fail_hip(ctx, e, "hipMalloc(memory of ejoin_embed.h)");
   }
   ctx->embed_bytes = bytes;
+  return EJOIN_OK;
+}
+
+// ... for a call on stream st.
+inline int ensure_embed(ejoin_ctx* ctx, int64_t bytes, hipStream_t st) {
+  EJ_RC(ensure_embed(ctx, bytes));
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st, &capture) != hipSuccess) (void)hipGetLastError();  // (the launches will say what is wrong with the stream)
+  if (capture != hipStreamCaptureStatusNone) ctx->embed_captured = true;
   return EJOIN_OK;
 }
 

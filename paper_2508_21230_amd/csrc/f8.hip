@@ -1187,7 +1187,7 @@ int launch_product(ejoin_ctx* ctx, const ejoin_f8_rows* A, const ejoin_f8_rows* 
   }
   a.tiles_n = (uint32_t)((a.n + 127) / 128);
   if (splits == 1) return launch_tiles<float, 2, 2>(ctx, A, B, a, 1, st);
-  EJ_RC(ensure_embed(ctx, parts_at + splits * tiles * (TILE * 128 * 4)));
+  EJ_RC(ensure_embed(ctx, parts_at + splits * tiles * (TILE * 128 * 4), st));
   a.parts = reinterpret_cast<float*>(ctx->embed + parts_at);  // (pieces are joined in FP32, whatever the results are rounded to then)
   EJ_RC((launch_tiles<float, 2, 2>(ctx, A, B, a, splits, st)));
   with_type(type, [&](auto t) {
@@ -1260,7 +1260,7 @@ int ejoin_f8_scores(ejoin_ctx* ctx, const void* X, int32_t xtype, int64_t m, int
   if (few(m, B->d)) return launch_few(ctx, X, nullptr, xtype, m, ldx, 0, B, scale, C, type, ldc, st);
   const int64_t width = up(B->d, BLOCK), scales = up(f8_blocks(B->d), 4), bytes = up(m * (width + scales), 256);
   // room for the splits' results as well: growing in between would free what the first launch writes
-  EJ_RC(ensure_embed(ctx, bytes + EJOIN_F8_PRODUCT_BYTES));
+  EJ_RC(ensure_embed(ctx, bytes + EJOIN_F8_PRODUCT_BYTES, st));
   const ejoin_f8_rows A{ctx->embed, ctx->embed + m * width, width, scales, m, B->d, EJOIN_E4M3};
   EJ_RC(launch_quantize(ctx, X, xtype, m, B->d, ldx, &A, nullptr, st));
   return launch_product(ctx, &A, B, scale, C, type, ldc, bytes, st);

@@ -709,7 +709,7 @@ int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, i
     EJ_TRY(hipGetLastError());
     return EJOIN_OK;
   }
-  EJ_RC(ensure_embed(ctx, 2 * list + counts + group_counts + pieces * 2 * width * 4));
+  EJ_RC(ensure_embed(ctx, 2 * list + counts + group_counts + pieces * 2 * width * 4, st));
   uint2* lists[2] = {reinterpret_cast<uint2*>(ctx->embed), reinterpret_cast<uint2*>(ctx->embed + list)};
   g.parts = reinterpret_cast<float*>(ctx->embed + 2 * list + counts + group_counts);
   SortArgs s;
