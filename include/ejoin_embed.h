@@ -37,7 +37,9 @@ int ejoin_embed_reserve(ejoin_ctx* ctx, int64_t bytes);
  * A row of d coordinates is cut into blocks of 128.  Block b holds x[k] as the nearest (ties to even) 8-bit value of
  * x[k] * 2^-e, 2^e the least power of two that brings the block's largest finite magnitude into the format's range (448 for
  * E4M3, 57344 for E5M2); e + 127 is the block's scale byte, cut off at 0 (and 127 for a block of zeros).  So no value
- * saturates, and multiplying by a scale never rounds.  NaN stays NaN; an infinity becomes NaN in E4M3 and stays one in E5M2.
+ * saturates, and multiplying by a scale never rounds; only magnitudes from 1.9375 * 2^127 on (from 1.875 * 2^127 in E5M2), FP32's and BF16's lowest value among
+ * them, which would round up to 2^128, are held as the value below it, so that whatever is finite stays a finite FP32 value.
+ * NaN stays NaN; an infinity becomes NaN in E4M3 and stays one in E5M2.
  *   values  n rows of roundup(d, 128) bytes, row stride ld (a multiple of 128, at most 2^23), 128-byte aligned; coordinates d and up are zero
  *   scales  n rows of roundup(ceil(d / 128), 4) bytes, row stride ld_scales (a multiple of 4, at most 2^24), 4-byte aligned;
  *           bytes past the last block hold 127 */

@@ -77,3 +77,36 @@ def test_columns_of_so_many_rows_are_refused(ej):
     with pytest.raises(pkg.EJoinError):
         ej.quantize_f8_both(x)
     assert ej.quantize_f8(x[:-1], columns=True).n == 2
+
+
+@pytest.mark.parametrize("form,most", [("e4m3", 1.875), ("e5m2", 1.75)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_largest_values_stay_finite(ej, form, most, dtype):
+    """Held as the largest value of the format below 2^128, by rows, by columns and within the call; products with zeros are zero."""
+    m, d = 140, 300
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((m, d), generator=gen, device="cuda").to(dtype)
+    top = torch.finfo(dtype).max
+    x[3, 7], x[5, 130:140], x[9], x[11, 299] = -top, top, -top, 1.76 * 2.0 ** 127
+    want = x[[3, 5, 9, 11]].double()
+    rows, columns = ej.quantize_f8_both(x, form)
+    for q in (rows, ej.quantize_f8(x, form)):
+        got = q.float()
+        assert torch.isfinite(got).all()
+        assert got[3, 7] == -most * 2.0 ** 127 and (got[5, 130:140] == most * 2.0 ** 127).all() and (got[9] == -most * 2.0 ** 127).all() and got[11, 299] == 1.75 * 2.0 ** 127
+        assert (got[3, :7] == 0).all() and (got[3, 128:].double() - want[0, 128:]).abs().max() < 0.3  # (other blocks are as they were)
+    for q in (columns, ej.quantize_f8(x, form, columns=True)):
+        got = q.float()
+        assert torch.isfinite(got).all() and got[7, 3] == -most * 2.0 ** 127 and (got[:, 9] == -most * 2.0 ** 127).all() and got[299, 11] == 1.75 * 2.0 ** 127
+    y = torch.randn((200, d), generator=gen, device="cuda") * 2.0 ** -40
+    y[:, 7] = 0.0
+    y[::2] = 0.0
+    b = ej.quantize_f8(y)
+    for a in (rows, pkg.F8Rows(rows.values[:20], rows.scales[:20], d, form)):
+        exact = a.float().double() @ b.float().double().T.contiguous()
+        size = a.float().double().abs() @ b.float().double().abs().T.contiguous()
+        for out in (torch.float32, torch.bfloat16):
+            got = ej.product_f8(a, b, out_dtype=out).double()
+            assert ((got - exact).abs() <= (302 * 2.0 ** -23 + (0.0 if out == torch.float32 else 2.0 ** -8 + 2.0 ** -10)) * size).all()
+        assert torch.equal(ej.scores_f8(x[:a.n], b), ej.product_f8(ej.quantize_f8(x[:a.n]), b))
+        assert torch.isfinite(ej.scores_f8(x[:a.n], b)).all()
