@@ -63,8 +63,10 @@ int ejoin_f8_quantize(ejoin_ctx* ctx, const void* X, int32_t type, int64_t n, in
 
 /* C[i][j] = scale * sum_k a_ik b_jk for the rows of A and of B (A->d = B->d), summed on the matrix cores block by block in
  * ascending order of k (in several pieces of that order, added up in it, where there are few tiles), rounded once to `type`.
- * FP32 results are sums in FP32 of the exact products.  For 16-bit results the 8-bit matrix cores
- * are used, whose sums of eight products keep no more than 13 bits below the largest of them: some 1.5e-5 of the result's norm.
+ * FP32 results are sums in FP32 of the exact products (of values held; those below 2^-126 are taken to the nearest 2^-133).  So are 16-bit results before
+ * they are rounded, where A has up to 64 rows of up to 1,024 coordinates (48 of 1,280, 32 of 2,048, 16 of 4,096) or where k is cut into pieces.  Other 16-bit
+ * results come from the 8-bit matrix cores, whose sums of eight products keep no more than 13 bits below the largest of them: some 1.5e-5 of the result's norm,
+ * up to 2^-10 of sum |a b| where sums cancel.  A row's bits may thus differ with the rows beside it; FP32 results are the call for sums that cancel.
  * C: A->n x B->n, row stride ldc; rows that are 16-byte aligned are written faster than others.
  * Formats may differ.  Works in at most EJOIN_F8_PRODUCT_BYTES of the context's memory. */
 #define EJOIN_F8_PRODUCT_BYTES (128ll << 20)

@@ -388,6 +388,8 @@ class EJoin:
         return out
 
     # ------------------------------------------------------------------ operators around a learnt table (ejoin_embed.h)
+    # Results carry no autograd graph, whether or not an input requires gradients: backward passes are calls of their own (lookup_grad, distill_grad,
+    # distill_with_grad, products of quantize_f8_both), which a torch.autograd.Function of the caller's puts together.
     def embed_reserve(self, nbytes: int):
         """Grow the memory that the operators below work in ahead of time."""
         self._check(self._lib.ejoin_embed_reserve(self._h, int(nbytes)), self._h)
@@ -464,7 +466,8 @@ class EJoin:
         return C.byref(x._c)
 
     def product_f8(self, A: F8Rows, B: F8Rows, scale: float = 1.0, out_dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
-        """scale * (rows of A) . (rows of B): (A.n, B.n), summed in FP32 and rounded once."""
+        """scale * (rows of A) . (rows of B): (A.n, B.n), rounded once.  FP32 results are sums in FP32; for 16-bit ones most sizes are summed on the
+        8-bit matrix cores, which keep fewer bits of sums that cancel (ejoin_f8_product says which)."""
         a, b = self._f8(A, "A"), self._f8(B, "B")
         if A.d != B.d:
             raise EJoinError("A and B must have the same number of coordinates")
@@ -530,7 +533,8 @@ class EJoin:
 
     def distill_grad(self, Z: torch.Tensor, lse: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, weights: torch.Tensor, temperature: float = 1.0,
                      out: torch.Tensor | None = None) -> torch.Tensor:
-        """The gradient of sum(weights * loss) with respect to Z, of Z's type; `out` may be Z."""
+        """The gradient of sum(weights * loss) with respect to Z, of Z's type; `out` may be Z.  It goes by an lse in float32, which limits it where |lse|
+        is large (ejoin_distill_grad); distill_with_grad does not."""
         t, v, ldz, ztype = self._matrix(Z, "Z")
         pi, itype, pt, k, ldi = self._lists(ids, teacher, t)
         out, lddz, otype = self._out(out, t, v, Z.dtype)
