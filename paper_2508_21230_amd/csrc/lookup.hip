@@ -165,7 +165,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scan_groups(const SortArg
   a.groups[(int64_t)groups * DIGITS + threadIdx.x] = exclusive_sum(all, scratch);
 }
 
-template <typename I, bool FIRST>
+template <typename I, bool FIRST, bool SCANNED>
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(const SortArgs a) {
   constexpr int WAVES = SORT_THREADS / 64;
   __shared__ uint32_t at[WAVES][DIGITS];  // a wavefront's count of a digit so far, then where its first one goes
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_scatter(const SortArgs a)
   __syncthreads();
   // thread = digit: its places in all blocks and in those before this one, and in the block's wavefronts
   uint32_t to;
-  if (a.groups) {
+  if (SCANNED) {
     const uint32_t groups = (a.blocks + SCAN_BLOCKS - 1) / SCAN_BLOCKS;
     to = a.counts[(int64_t)blockIdx.x * DIGITS + threadIdx.x] + a.groups[(int64_t)(blockIdx.x / SCAN_BLOCKS) * DIGITS + threadIdx.x] +
          a.groups[(int64_t)groups * DIGITS + threadIdx.x];
@@ -721,21 +721,21 @@ int ejoin_lookup_grad(ejoin_ctx* ctx, const void* dY, int32_t type, int64_t t, i
     s.items = lists[pass & 1], s.items_out = lists[1 - (pass & 1)];
     s.shift = pass * digit;
     const dim3 grid((unsigned)blocks), block(SORT_THREADS);
-    auto scan = [&] {
-      if (!groups) return;
-      hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)groups), block, 0, st, s);
-      hipLaunchKernelGGL(k_sort_scan_groups, dim3(1), block, 0, st, s, (uint32_t)groups);
+    auto sort = [&](auto count, auto scatter, auto scatter_scanned) {
+      hipLaunchKernelGGL(count, grid, block, 0, st, s);
+      if (groups) {
+        hipLaunchKernelGGL(k_sort_scan, dim3((unsigned)groups), block, 0, st, s);
+        hipLaunchKernelGGL(k_sort_scan_groups, dim3(1), block, 0, st, s, (uint32_t)groups);
+      }
+      hipLaunchKernelGGL(groups ? scatter_scanned : scatter, grid, block, 0, st, s);
     };
     if (pass == 0) {
       with_index(token_type, [&](auto i) {
-        hipLaunchKernelGGL((k_sort_count<decltype(i), true>), grid, block, 0, st, s);
-        scan();
-        hipLaunchKernelGGL((k_sort_scatter<decltype(i), true>), grid, block, 0, st, s);
+        typedef decltype(i) I;
+        sort(&k_sort_count<I, true>, &k_sort_scatter<I, true, false>, &k_sort_scatter<I, true, true>);
       });
     } else {
-      hipLaunchKernelGGL((k_sort_count<int32_t, false>), grid, block, 0, st, s);
-      scan();
-      hipLaunchKernelGGL((k_sort_scatter<int32_t, false>), grid, block, 0, st, s);
+      sort(&k_sort_count<int32_t, false>, &k_sort_scatter<int32_t, false, false>, &k_sort_scatter<int32_t, false, true>);
     }
     EJ_TRY(hipGetLastError());
     g.items = s.items_out;
