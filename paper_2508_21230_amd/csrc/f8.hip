@@ -56,20 +56,22 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(c, d, lo, true);
 }
 
-// Four values of a block with this scale byte, scaled, as bytes.  The largest FP32 values, above 1.9375 * 2^127, would round up to 2^128, which is
+// Eight values of a block with this scale byte, scaled, as bytes.  The largest FP32 values, above 1.9375 * 2^127, would round up to 2^128, which is
 // no FP32 value and an infinity to whatever expands the rows: they are held as the format's value below it.
 template <int FMT>
-__device__ __forceinline__ uint32_t scaled4(float a, float b, float c, float d, uint32_t byte) {
+__device__ __forceinline__ uint2 scaled8(const float (&x)[8], uint32_t byte) {
   constexpr uint32_t TOP = FMT == EJOIN_E4M3 ? 247u : 240u;
   constexpr float MOST_AT_TOP = FMT == EJOIN_E4M3 ? 240.f : 28672.f;
   const float f = inverse_scale(byte);
-  float x[4] = {a * f, b * f, c * f, d * f};
-  if (byte == TOP) {
+  float y[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (fabsf(x[i]) > MOST_AT_TOP && fabsf(x[i]) < INFINITY) x[i] = copysignf(MOST_AT_TOP, x[i]);
+  for (int i = 0; i < 8; ++i) y[i] = x[i] * f;
+  if (__builtin_expect(byte == TOP, 0)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (fabsf(y[i]) > MOST_AT_TOP && fabsf(y[i]) < INFINITY) y[i] = copysignf(MOST_AT_TOP, y[i]);
   }
-  return pack4<FMT>(x[0], x[1], x[2], x[3]);
+  return {pack4<FMT>(y[0], y[1], y[2], y[3]), pack4<FMT>(y[4], y[5], y[6], y[7])};
 }
 
 struct QuantArgs {
@@ -176,7 +178,7 @@ __device__ __forceinline__ uint32_t largest_of_16(uint32_t m) {
 }
 
 // Whether a block with this maximum (FP32 bits) takes the long way: values that are not finite are to be left out of the maximum, values above
-// 1.75 * 2^127 may be too large (see scaled4), and the scale of the smallest blocks is no normal number.
+// 1.75 * 2^127 may be too large (see scaled8), and the scale of the smallest blocks is no normal number.
 __device__ __forceinline__ bool unusual(uint32_t max_bits, uint32_t byte) { return max_bits > 0x7F600000u || byte == 0; }
 
 // Two values of a pair of words (16 bits) or two words (FP32), scaled, into the lower or upper half of q.
@@ -222,8 +224,10 @@ __global__ __launch_bounds__(256) void k_quantize_rows(const QuantArgs a) {
       for (int j = 0; j < 8; ++j) m = max(m, finite_bits(x[i].get(j)));
       m = largest_of_16<float>(m);
       byte = scale_byte<FMT>(m);
-      q.x = scaled4<FMT>(x[i].get(0), x[i].get(1), x[i].get(2), x[i].get(3), byte);
-      q.y = scaled4<FMT>(x[i].get(4), x[i].get(5), x[i].get(6), x[i].get(7), byte);
+      float y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = x[i].get(j);
+      q = scaled8<FMT>(y, byte);
     } else {
       const float f = __builtin_bit_cast(float, byte << 23);
       constexpr int S = sizeof(T) == 4 ? 2 : 1;  // words of a pair
@@ -282,8 +286,10 @@ __global__ __launch_bounds__(256) void k_quantize_tile(const QuantArgs a) {
         for (int j = 0; j < 8; ++j) m = max(m, finite_bits(x[i].get(j)));
         m = largest_of_16<float>(m);
         byte = scale_byte<FMT>(m);
-        q.x = scaled4<FMT>(x[i].get(0), x[i].get(1), x[i].get(2), x[i].get(3), byte);
-        q.y = scaled4<FMT>(x[i].get(4), x[i].get(5), x[i].get(6), x[i].get(7), byte);
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = x[i].get(j);
+        q = scaled8<FMT>(y, byte);
       } else {
         const float f = __builtin_bit_cast(float, byte << 23);
         q.x = scaled2<FMT, T, true>(scaled2<FMT, T, false>(0, x[i].w[0], x[i].w[S - 1], f), x[i].w[S], x[i].w[2 * S - 1], f);
@@ -348,7 +354,7 @@ __global__ __launch_bounds__(256) void k_quantize_tile(const QuantArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = PER == 1 ? __builtin_bit_cast(float, x[i].w[j]) : Octet<T>::value(x[i].w[j], h);
         const uint32_t byte = scale_byte<FMT>(PER == 1 ? exact[j] : (h ? exact[2 * j + 1 < 8 ? 2 * j + 1 : 0] : exact[2 * j < 8 ? 2 * j : 0]));
-        put_column(PER * j + h, uint2{scaled4<FMT>(y[0], y[1], y[2], y[3], byte), scaled4<FMT>(y[4], y[5], y[6], y[7], byte)}, byte);
+        put_column(PER * j + h, scaled8<FMT>(y, byte), byte);
       }
     }
   } else {
@@ -940,7 +946,7 @@ __device__ __forceinline__ void few_fill(const FewArgs& a, uint8_t* lds) {  // f
 #pragma unroll
       for (int s = 1; s < 16; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
       const uint32_t byte = scale_byte<EJOIN_E4M3>(m);
-      const uint2 q{scaled4<EJOIN_E4M3>(x[i][0], x[i][1], x[i][2], x[i][3], byte), scaled4<EJOIN_E4M3>(x[i][4], x[i][5], x[i][6], x[i][7], byte)};
+      const uint2 q = scaled8<EJOIN_E4M3>(x[i], byte);
       few_put<MT>(lds, row[i], block[i], lane16, expand8<EJOIN_E4M3>(q, scale_of(byte)));
     }
   }
