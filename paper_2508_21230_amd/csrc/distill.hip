@@ -143,7 +143,9 @@ struct FromLse {
   __device__ __forceinline__ float operator()(float z) const { return factor * exp2_of((z * inv_t - lse) * LOG2E); }
 };
 
-// The entries of [from, to) once the rest of the gradient is written: each writes the value for all entries with its id.
+// The entries of [from, to) once the rest of the gradient is written: each writes the value for all entries with its id, for which it looks through the
+// list.  That grows as the square of the list: 4,096 rows of 4,099 BF16 scores with lists of 1,024, loss and gradient, 605 us, where the bytes are 14; with lists
+// of up to 100 or so it is lost beside the row.
 template <typename T, typename Q>
 __device__ __forceinline__ void put_entries(const DistillArgs& a, T* dz, int64_t from, int64_t to, const List& list, const Q& weighted_q, float weight, int threads) {
   for (int i = threadIdx.x; i < a.k; i += threads) {
@@ -161,7 +163,10 @@ __device__ __forceinline__ void put_entries(const DistillArgs& a, T* dz, int64_t
 // All of a row's loads are under way together, the first wavefront sees to its list meanwhile.  One barrier for the statistics; one
 // between the gradient and the entries' places in it.  Bound by the memory: loss and gradient of 4,096 rows of 50,021 BF16 scores 190 us for the 822 MB that are read
 // and written once, 4.3 TB/s.  (Scores kept as FP32 take twice the registers and leave one workgroup a CU: 299 us.  Rows read a second time for the gradient: 359.)
-// Threads and pieces: as few registers a thread as bring two rows or more to a CU.
+// Threads and pieces: as few registers a thread as bring two rows or more to a CU.  13 pieces of 16-bit scores take 82 registers by themselves, two more
+// than leave room for a third workgroup: held to those, loss and gradient of 4,096 rows of 41,000, 45,001 and 50,021 176, 194 and 220 us -> 153, 184 and
+// 205, the two calls of one each unchanged.  Ten pieces need 68 and have three workgroups anyway; 16 need 95 (held to 80: loss of 4,096 x 60,001 146 ->
+// 130 us, both 246 -> 273); a second workgroup of 1,024 threads would have to do with 64.
 // Eight scores as the words they are in memory: the compiler keeps 16-bit ones two to a register only where it sees no more than that.
 template <typename T>
 struct Words {
@@ -286,7 +291,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 && PIECES == 13 ? 6 : THREA
 // ------------------------------------------------------------------------------------------
 // The statistics of a piece, by eight wavefronts; a ninth sees to the list meanwhile, and if its workgroup is the last of the row to
 // be done, joins the pieces' statistics and works out the loss.  5 rows of 1,000,000 FP32 scores (20 MB) 11.2 us, of which a launch and the join are some 7.
-// (A list that the wavefronts see to before or after the scores: 15.7 us.)
+// (A list that the wavefronts see to before or after the scores: 15.7 us.)  Rows that no workgroup holds, loss and gradient, read twice: 512 of 128,256 FP32
+// 193 us (76 and 114 for the launches, 788 MB: 4.1 TB/s), 2,048 of 151,936 BF16 439.
 template <typename T>
 __global__ __launch_bounds__(LONG_THREADS + 64) void k_distill_long(const DistillArgs a) {
   __shared__ List list;
@@ -442,6 +448,8 @@ void split_rows(const ejoin_ctx* ctx, DistillArgs& a) {
 // 16-bit scores, whole and in pieces: forward, 128 rows of 20,011 8.9 and 8.7 us, of 40,009 9.7 and 8.9, of 130,003 20.9 and
 // 16.8, 256 of 40,009 10.7 and 12.0; gradient, 128 of 40,009 12.7 and 10.6, of 130,003 24.7 and 16.5; both, where pieces are read twice, 32 of 40,009 13.8 and
 // 16.1, of 65,521 20.0 and 16.5, 128 of 90,001 23.5 and 26.2.
+// FP32 ones, in graphs, which adds 6 us: forward, 1 row of 33,001 13.0 and 12.2, 128 of 33,001 16.7 and 14.9, of 65,521 17.3 and 16.5, 256 of 40,009 17.3 and 18.3;
+// gradient, 128 of 33,001 19.6 and 18.6, of 65,521 26.1 and 23.2; both, 32 of 33,001 18.2 and 20.6, of 65,521 23.3 and 21.7, 64 of 65,521 25.8 and 25.7, 128 29.0 and 31.9.
 template <bool BOTH>
 bool few_long(const ejoin_ctx* ctx, int64_t t, int64_t v) {
   return BOTH ? v > 53248 && t <= ctx->num_cu / 4 : v > 32768 && t <= ctx->num_cu / 2;

@@ -73,14 +73,17 @@ __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
 // ascending order.  Then pieces of CHUNK sorted places are summed side by side, whatever rows they belong to: frequent tokens make no
 // workgroup's work longer.  A row whose places lie in one piece is written at once; one that goes on in the next piece leaves sums
 // that k_grad_join adds up in their order.
-// 300,007 tokens, frequencies as 1 / rank, of 100,000 rows of 384, FP16 into FP32: 155 us; of that the sort 35, the sums 102 (385 MB, 3.8 TB/s: rows of 768 bytes
-// in the order of the table), the long runs 25.  Pieces of 16, 32 and 64 places: 186, 164 and 166 us; 20,000 of 50,000 x 128: 121, 122, 133.
+// 300,007 tokens, frequencies as 1 / rank, of 100,000 rows of 384, FP16 into FP32: 156 us; of that the sort 34, the sums 102 (385 MB, 3.8 TB/s: rows of 768 bytes
+// in the order of the table), the long runs 20.  Pieces of 16, 32 and 64 places, in graphs: 183, 161 and 160 us; 20,000 of 50,000 x 128: 50, 57, 76; even
+// frequencies 127, 127, 137 and 43, 43, 57.  Few tens of thousands of tokens are bound by the six launches that wait for each other.
+// Places without a token sort last and are read like others, their sum is dropped: 300,000 tokens of which half are none take as long as if all were there.
 constexpr int DIGIT_BITS = 9;
 constexpr int DIGITS = 1 << DIGIT_BITS;
 constexpr int SORT_THREADS = 512;  // (as many as there are digits)
 constexpr int SORT_ITEMS = 4;
 constexpr int SORT_BLOCK = SORT_THREADS * SORT_ITEMS;
 constexpr int CHUNK = 32;
+// (4,000,000 tokens, traced: counts 8 and 12 us, running sums 9 + 5 a pass, scatters 30 and 19.)
 // From SCAN_FROM blocks on their counts are turned into running sums first, in groups of SCAN_BLOCKS; below, every block adds up the counts of all
 // others for itself, which is two launches less but grows as their square.  The gradient of 400,000, 500,000, 600,000 and 4,000,000 tokens of 100,000
 // rows of 64 with running sums 74, 77, 84 and 404 us, without 71, 77, 92 and 963; of 300 rows of 16 57, 60, 64, 169 and 54, 59, 67, 444.
@@ -488,7 +491,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(const GradArgs a, co
 // A workgroup owns SMALL_ROWS rows of the table or fewer.  It reads all tokens (from the L2: there are few), keeps those of its
 // rows in the LDS, puts them in the order of (row, place) and writes its rows.  A row of few places is one group of lanes'; one of
 // many is shared by all of them, whose sums are added up in order.  Bound by the launch and the latency of three dependent reads: 2,011 tokens of
-// 4,096 rows of 128 11 us.  8,000 tokens of 100,000 x 256 57 us, by the sort 67; of 2,000 x 96 25 and 49.
+// 4,096 rows of 128 11 us.  8,000 tokens of 100,000 x 256 57 to 62 us, by the sort 67; of 2,000 x 96 25 and 49.  Larger tables: every workgroup looks
+// through all tokens before it writes its rows, most of them zeros (1,000 of 50,000 x 300 38 us for 61 MB).
 constexpr int SMALL_ROWS = 64;
 constexpr int SMALL_ALONE = 32;  // places of a row that one group sums
 constexpr int SMALL_PLACES = 8192;  // at most
