@@ -73,8 +73,8 @@ __global__ __launch_bounds__(256) void k_lookup(const LookupArgs a) {
 // ascending order.  Then pieces of CHUNK sorted places are summed side by side, whatever rows they belong to: frequent tokens make no
 // workgroup's work longer.  A row whose places lie in one piece is written at once; one that goes on in the next piece leaves sums
 // that k_grad_join adds up in their order.
-// 300,007 tokens, frequencies as 1 / rank, of 100,000 rows of 384, FP16 into FP32: 156 us; of that the sort 34, the sums 102 (385 MB, 3.8 TB/s: rows of 768 bytes
-// in the order of the table), the long runs 20.  Pieces of 16, 32 and 64 places, in graphs: 183, 161 and 160 us; 20,000 of 50,000 x 128: 50, 57, 76; even
+// 300,007 tokens, frequencies as 1 / rank, of 100,000 rows of 384, FP16 into FP32: 157 us; of that the sort 34, the sums 102 (385 MB, 3.8 TB/s: rows of 768 bytes
+// in the order of the table), the long runs 22.  Pieces of 16, 32 and 64 places, in graphs: 183, 161 and 160 us; 20,000 of 50,000 x 128: 50, 57, 76; even
 // frequencies 127, 127, 137 and 43, 43, 57.  Few tens of thousands of tokens are bound by the six launches that wait for each other.
 // Places without a token sort last and are read like others, their sum is dropped: 300,000 tokens of which half are none take as long as if all were there.
 constexpr int DIGIT_BITS = 9;
@@ -422,9 +422,11 @@ __global__ __launch_bounds__(256) void k_grad_sum(const GradArgs a) {
 
 // Long runs: a workgroup looks through JOIN_PIECES pieces for runs that begin in them, and adds up the parts of each, every
 // group of lanes those of some consecutive pieces, then their sums in order.
-// (512 threads and eight pieces, 1,024 and sixteen, 256 and four: 300,007 tokens of 100,000 x 384, all of it, 155, 156 and 159 us; 400,000 of 2,000 x 64 80, 93 and 75.)
-constexpr int JOIN_THREADS = 512;
-constexpr int JOIN_PIECES = 8;
+// 256 threads and four pieces, 512 and eight, 1,024 and sixteen, whole gradients in graphs, frequencies even or as 1 / rank: 400,000 tokens of 2,000 x 64 71, 78,
+// 87 and 81, 87, 95 us; 1,000,000 of 5,000 x 128 131, 148, 173 and 146, 146, 166; 200,000 of 1,000 x 300 89, 96, 104 and 117, 113, 118; 100,000 of 100,000 x 256
+// 64, 64, 64 and 75, 77, 81; 300,007 of 100,000 x 384 127, 127, 127 and 162, 158, 161.
+constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_PIECES = 4;
 template <typename O>
 __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(const GradArgs a, const uint32_t first_block) {
   __shared__ float sums[JOIN_THREADS * 8];
