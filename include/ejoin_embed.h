@@ -109,7 +109,7 @@ int ejoin_embed_status(ejoin_ctx* ctx, int* status);
  * in FP32, rounded once.  sum_i p_i is 1, or 0 for a row without entries: its loss and gradient are zero, whatever its scores
  * hold.  An id may stand in a list more than once.  Scores of -infinity are left out (q = 0); one that an entry names
  * makes the loss infinite; a NaN or +infinity makes the row's loss, lse and gradient NaN.  Of a row that holds nothing but
- * -infinity all q are 0.
+ * -infinity all q are 0.  A NaN or +infinity among the entries' logits makes the row's loss NaN, and the gradient where its entries point.
  *   Z, dZ    t x v, row strides ldz, lddz, both of type ztype; dZ may be Z
  *   ids      t x k, row stride ldi;  teacher FP32, t x k, row stride ldi
  *   0 <= k <= EJOIN_DISTILL_MAX_ENTRIES;  1 <= v < 2^31;  t = 0 enqueues nothing;  temperature finite and at least 4.24e-39 (log2(e) / T is finite) */
