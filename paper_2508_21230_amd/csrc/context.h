@@ -17,7 +17,7 @@ static_assert(EJ_TOKEN_STATUS >= EJ_BATCH_COUNTER + 2 && EJ_TOKEN_STATUS < EJ_ST
 
 // Device memory one call works in: either the context's own (grown on demand) or a carving of the static scratch.
 struct Workspace {
-  uint32_t* status;  // status block, EJ_STATUS_WORDS words (see below and k_reset)
+  uint32_t* status;  // status block, EJ_STATUS_WORDS words (see above and k_reset)
   float* s;          // norms (4 B per point)
   uint32_t* maxima;  // behind them, small problems and the dense-tile call: largest norms of the norm kernels' workgroups (at most one per NORM_POINTS points)
   uint4* Xp;         // packed copy of X plus the augmentation k-block
